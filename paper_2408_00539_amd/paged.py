@@ -34,6 +34,8 @@ block table row and length.
 
 from __future__ import annotations
 
+import contextlib
+
 import numpy as np
 
 from . import ops
@@ -115,15 +117,34 @@ class PageAllocator:
 
     def trim(self, slot, window, sinks):
         """Free the pages of ``slot`` that no token from position ``lens[slot]``
-        on sees: wholly behind its window, without a sink."""
+        on sees: wholly behind its window, without a sink. They are the last
+        free pages to be used. Returns what ``untrim`` takes."""
         first = -(-int(sinks) // self.page_size)
         end = max(int(self.lens[slot]) - int(window) + 1, 0) // self.page_size
-        done = max(first, self._trimmed[slot][1])
-        for i in range(done, min(end, len(self.held[slot]))):
-            self._drop(self.held[slot][i])
-            self.held[slot][i] = -1
-            self.table[slot, i] = 0
-            self._trimmed[slot] = (first, i + 1)
+        before = self._trimmed[slot]
+        done = max(first, before[1])
+        pages = self.held[slot][done:end]
+        for i, page in enumerate(pages, done):
+            self.refs[page] -= 1
+            self._put(slot, i, -1)
+        if pages:
+            self._trimmed[slot] = (first, done + len(pages))
+            self._free[:0] = [page for page in pages if self.refs[page] == 0]
+        return slot, done, pages, before
+
+    def untrim(self, trimmed, lost=()):
+        """Undo ``trim`` (its result), but for the pages in ``lost`` (their
+        values are gone) and those before them."""
+        slot, done, pages, before = trimmed
+        for i in reversed(range(len(pages))):
+            page = pages[i]
+            if page in lost:
+                return
+            if self.refs[page] == 0:
+                self._free.remove(page)
+            self.refs[page] += 1
+            self._put(slot, done + i, page)
+            self._trimmed[slot] = (self._trimmed[slot][0], done + i) if i else before
 
     def fork(self, slot, new_slot):
         """``new_slot``, which must be empty, holds the same positions in the
@@ -166,7 +187,7 @@ class PageAllocator:
 
     def _put(self, slot, at, page):
         self.held[slot][at] = page
-        self.table[slot, at] = page
+        self.table[slot, at] = max(page, 0)
 
     def compact(self):
         """Give the n pages in use the indices 0 .. n - 1. Returns (n, old
@@ -217,6 +238,10 @@ class PagedKVCache:
         """Reserve pages for every slot or, if one request fails, for none
         (the pages reserved by this call go back to the pool). Returns the
         copies of shared pages that the appends need first."""
+        return [copy for _, copy in self._reserved(slots, lengths) if copy is not None]
+
+    def _reserved(self, slots, lengths):
+        """``_reserve_all`` with each slot and its copy or None."""
         if len(set(slots)) != len(slots):
             raise ValueError("a slot appears twice in one call")
         done = []
@@ -225,12 +250,15 @@ class PagedKVCache:
                 self.alloc.reserve(s, n)
                 done.append([s, None])
                 done[-1][1] = self.alloc.own_last(s)
-        except Exception:
-            for s, copy in reversed(done):
-                self.alloc.give_back(s, copy)
-                self._shrink(s)
+        except BaseException:
+            self._give_back(done)
             raise
-        return [copy for _, copy in done if copy is not None]
+        return done
+
+    def _give_back(self, done):
+        for s, copy in reversed(done):
+            self.alloc.give_back(s, copy)
+            self._shrink(s)
 
     def _shrink(self, slot):
         """Pages reserved past the slot's length return."""
@@ -239,13 +267,28 @@ class PagedKVCache:
             self.alloc._drop(held.pop())
             self.alloc.table[slot, len(held)] = 0
 
-    def _append_to(self, slots, lengths):
-        """Room for the slots' new lengths, with the pages behind the window
-        freed and shared pages that are written copied first."""
-        if self.window is not None:
-            for s in slots:
-                self.alloc.trim(s, self.window, self.sinks)
-        self._copy(self._reserve_all(slots, lengths))
+    @contextlib.contextmanager
+    def _appending(self, slots, new_lens):
+        """Around an append of ``new_lens`` tokens to ``slots``: room for them,
+        with the pages behind the window freed and shared pages that are written
+        copied first. If any of it or the append is refused, the slots are as
+        they were (but for pages behind the window that, the pool being short,
+        a shared page was copied over: they stay freed)."""
+        a, trimmed, done = self.alloc, [], []
+        try:
+            if self.window is not None:
+                for s in slots:
+                    trimmed.append(a.trim(s, self.window, self.sinks))
+            done = self._reserved(slots, [a.lens[s] + n for s, n in zip(slots, new_lens)])
+            self._copy([copy for _, copy in done if copy is not None])
+            yield
+        except BaseException:
+            self._give_back(done)
+            for t in reversed(trimmed):
+                a.untrim(t, [copy[1] for _, copy in done if copy is not None])
+            raise
+        for s, n in zip(slots, new_lens):
+            a.lens[s] += n
 
     def _copy(self, copies):
         import torch
@@ -268,42 +311,34 @@ class PagedKVCache:
         new_lens = [int(n) for n in new_lens]
         if len(new_lens) != len(slots) or min(new_lens, default=1) < 1:
             raise ValueError("one new length >= 1 per slot")
-        self._append_to(slots, [self.alloc.lens[s] + n for s, n in zip(slots, new_lens)])
-        tab, lens = self._views(slots)
-        cu = torch.tensor(np.concatenate([[0], np.cumsum(new_lens)]), dtype=torch.int32,
-                          device=self.device)
-        args = (q_new, k_new, v_new, self.k_pages, self.v_pages, tab, lens, cu, max(new_lens))
-        if self.window is None:
-            out = ops.prefill_paged(*args, seg_is_query, scale)
-        else:
-            out = ops.prefill_paged_window(*args, self.window, self.sinks, seg_is_query, scale)
-        for s, n in zip(slots, new_lens):
-            self.alloc.lens[s] += n
-        return out
+        with self._appending(slots, new_lens):
+            tab, lens = self._views(slots)
+            cu = torch.tensor(np.concatenate([[0], np.cumsum(new_lens)]), dtype=torch.int32,
+                              device=self.device)
+            args = (q_new, k_new, v_new, self.k_pages, self.v_pages, tab, lens, cu, max(new_lens))
+            if self.window is None:
+                return ops.prefill_paged(*args, seg_is_query, scale)
+            return ops.prefill_paged_window(*args, self.window, self.sinks, seg_is_query, scale)
 
     def decode(self, slots, q, k_new, v_new, scale=None, num_splits=0):
         """One answer token for each slot in ``slots``. Returns (o, lse)."""
         import torch
         slots = list(slots)
-        self._append_to(slots, [self.alloc.lens[s] + 1 for s in slots])
-        tab, lens = self._views(slots)
-        sizes = (self.alloc.capacity, q.shape[1], self.hkv, self.d)
-        if self.window is None:
-            need = ops.workspace_size(ops.ISM_OP_DECODE, len(slots), 0, *sizes, num_splits)
-        else:
-            need = ops.window_workspace_size(ops.ISM_OP_DECODE, len(slots), 0, 0, *sizes,
-                                             self.window, self.sinks, num_splits)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-        args = (q, k_new, v_new, self.k_pages, self.v_pages, tab, lens)
-        if self.window is None:
-            out = ops.decode_paged(*args, 0, scale, num_splits, workspace=self._ws)
-        else:
-            out = ops.decode_paged_window(*args, self.window, self.sinks, 0, scale, num_splits,
-                                          workspace=self._ws)
-        for s in slots:
-            self.alloc.lens[s] += 1
-        return out
+        with self._appending(slots, [1] * len(slots)):
+            tab, lens = self._views(slots)
+            sizes = (self.alloc.capacity, q.shape[1], self.hkv, self.d)
+            if self.window is None:
+                need = ops.workspace_size(ops.ISM_OP_DECODE, len(slots), 0, *sizes, num_splits)
+            else:
+                need = ops.window_workspace_size(ops.ISM_OP_DECODE, len(slots), 0, 0, *sizes,
+                                                 self.window, self.sinks, num_splits)
+            if self._ws is None or self._ws.numel() < need:
+                self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            args = (q, k_new, v_new, self.k_pages, self.v_pages, tab, lens)
+            if self.window is None:
+                return ops.decode_paged(*args, 0, scale, num_splits, workspace=self._ws)
+            return ops.decode_paged_window(*args, self.window, self.sinks, 0, scale, num_splits,
+                                           workspace=self._ws)
 
     def rollback(self, slot, length):
         self.alloc.rollback(slot, length, self.window)
