@@ -192,10 +192,18 @@ class PageAllocator:
     def compact(self):
         """Give the n pages in use the indices 0 .. n - 1. Returns (n, old
         indices, new indices) of the pages that move."""
+        n, src, dst = self.moves()
+        self.move(n, src, dst)
+        return n, src, dst
+
+    def moves(self):
+        """What ``compact`` returns, with nothing changed."""
         used = np.flatnonzero(self.refs > 0)
         n = len(used)
-        src = used[used >= n]
-        dst = np.flatnonzero(self.refs[:n] == 0)
+        return n, used[used >= n], np.flatnonzero(self.refs[:n] == 0)
+
+    def move(self, n, src, dst):
+        """Give the pages src, of n in use, the indices dst."""
         new = np.arange(self.num_pages)
         new[src] = dst
         for slot, held in enumerate(self.held):
@@ -205,7 +213,6 @@ class PageAllocator:
         self.refs[dst] = self.refs[src]
         self.refs[src] = 0
         self._free = list(range(self.num_pages - 1, n - 1, -1))
-        return n, src, dst
 
 
 class PagedKVCache:
@@ -353,6 +360,7 @@ class PagedKVCache:
     def compact(self):
         """Move the pages in use to the front of the pools; returns their
         number. (Block tables of earlier calls are out of date then.)"""
-        n, src, dst = self.alloc.compact()
+        n, src, dst = self.alloc.moves()
         self._copy([(int(s), int(t), self.alloc.page_size) for s, t in zip(src, dst)])
+        self.alloc.move(n, src, dst)
         return n

@@ -1,7 +1,8 @@
 """A paged cache's append that is refused, at whatever point, leaves every slot as
-it was: its pages, those behind its window, and how far it can be rolled back (no
-GPU: the calls fail a host check)."""
+it was: its pages, those behind its window, and how far it can be rolled back; so
+does a compaction (no GPU: the calls fail a host check)."""
 
+import numpy as np
 import pytest
 
 from paper_2408_00539_amd.paged import PagedKVCache, PoolExhausted
@@ -125,3 +126,12 @@ def test_a_trimmed_page_serves_the_same_call(monkeypatch):
         assert cache.prefill([0], None, None, None, [n]) == "o"
         check(cache.alloc)
     assert cache.lens[0] == 380 and len([p for p in cache.alloc.held[0] if p >= 0]) <= 3
+
+
+def test_compaction_that_cannot_copy_moves_nothing():
+    cache = _cache()
+    grow(cache.alloc, 0, 300)
+    grow(cache.alloc, 1, 300)
+    cache.release(0)
+    _unchanged(cache, cache.compact, ValueError)      # (pools that are not on a GPU)
+    assert np.array_equal(cache.alloc.compact()[2], np.arange(5))
