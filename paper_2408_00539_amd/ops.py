@@ -592,18 +592,20 @@ def decode_paged(q, k_new, v_new, k_pages, v_pages, block_table,
 
 # ------------------------------------------------------- windowed attention
 
-@functools.lru_cache(maxsize=256, typed=True)
-def window_workspace_size(op, batch=0, total_tokens=0, max_new=0, max_seqlen=0, hq=0, hkv=0,
-                          d=0, window=0, sinks=0, num_splits=0):
-    return int(lib().ism_attn_window_workspace_size(op, batch, total_tokens, max_new, max_seqlen,
-                                                    hq, hkv, d, window, sinks, num_splits))
-
-
 def _window(window, sinks):
     """Whole numbers in int32 (a window of any greater length hides no more)."""
     if int(window) != window or int(sinks) != sinks:
         raise ValueError(f"window and sinks must be whole numbers (got {window}, {sinks})")
-    return min(int(window), 2 ** 31 - 1), min(int(sinks), 2 ** 31 - 1)
+    return (max(min(int(window), 2 ** 31 - 1), -2 ** 31),
+            max(min(int(sinks), 2 ** 31 - 1), -2 ** 31))
+
+
+@functools.lru_cache(maxsize=256, typed=True)
+def window_workspace_size(op, batch=0, total_tokens=0, max_new=0, max_seqlen=0, hq=0, hkv=0,
+                          d=0, window=0, sinks=0, num_splits=0):
+    return int(lib().ism_attn_window_workspace_size(op, batch, total_tokens, max_new, max_seqlen,
+                                                    hq, hkv, d, *_window(window, sinks),
+                                                    num_splits))
 
 
 def _on_current(*tensors):

@@ -229,7 +229,7 @@ class PagedKVCache:
             raise ValueError(f"window {window} must be at least 1")
         if sinks < 0 or (sinks and window is None):
             raise ValueError(f"sinks {sinks} must be at least 0, and need a window")
-        self.window, self.sinks = window, sinks
+        self.window, self.sinks = (None, 0) if window is None else ops._window(window, sinks)
         self.alloc = PageAllocator(num_pages, page_size, slots, max_pages)
         self.hkv, self.d, self.device = hkv, d, device
         shape = (num_pages, hkv, page_size, d)
