@@ -647,6 +647,7 @@ dq_kernel(BwdArgs a, int hpw, int tiles, int slots) {
   constexpr int NKS = D / 16, NDB = D / 32, RB = D * 2, LA = 3;
   __shared__ DqSmem<D> sm;
   __shared__ uint32_t tab[kMaxTableSegs + 1];
+  __shared__ int few[WIN ? NWV : 1];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hf = lane >> 5;
@@ -793,13 +794,19 @@ dq_kernel(BwdArgs a, int hpw, int tiles, int slots) {
   // one over the root of the number of keys: against the rounding of dS that
   // counts below about 128 keys (relative error of dQ and dK in norm, bf16
   // gradients, of a window of 4, 32, 100 keys: 0.0030, 0.0025, 0.0025; so 0.0024).
-  // Workgroups whose first row sees no more walk up to four tiles once before the
-  // steps; rows whose keys end there take it.
+  // Workgroups with a row that sees no more (the last ones of a query segment see
+  // fewer than its first) walk up to four tiles once before the steps; rows whose
+  // keys end there take it: among them all that see at most 128, since the list
+  // starts at most 127 keys before a row's window.
   if constexpr (WIN) {
+    const int seen = lim_r - max(lo_r, s) + 1 + max(min(send, lo_r) - s, 0);
+    const bool wave_few = __builtin_amdgcn_ballot_w64(seen <= 2 * kBK) != 0;
+    if (lane == 0) few[wave] = wave_few;
     __syncthreads();
-    const int first_hi = __builtin_amdgcn_readfirstlane(
-        (a.lim ? a.lim[q0] : seg_lim(tab, a.num_segs, q0)) - wl.shift);
-    const int np = first_hi - s < 2 * kBK ? min(ntiles, 4) : 0;
+    bool any = false;
+#pragma unroll
+    for (int w = 0; w < NWV; ++w) any |= few[w] != 0;
+    const int np = any ? __builtin_amdgcn_readfirstlane(min(ntiles, 4)) : 0;
     float acc = 0.f, psum = 0.f;
 #pragma unroll 1
     for (int t = 0; t < np; ++t) {
