@@ -233,9 +233,13 @@ int32_t window_keys(const Window &w, int32_t new_rows, int32_t keys) {
   return n < keys ? (int32_t)n : keys;
 }
 
-size_t bwd_far_bytes(int32_t batch, int32_t max_seqlen, int32_t hkv, int32_t d, const Window &w) {
+// Partials of the sinks; near: with the slot of the rows inside the window.
+size_t bwd_far_bytes(int32_t batch, int32_t total, int32_t max_seqlen, int32_t hkv, int32_t d,
+                     const Window &w, bool near) {
   const int parts = ism::bwd_far_parts(batch, max_seqlen, hkv, w.size, w.sinks);
-  return parts ? align_up((size_t)2 * (1 + parts) * batch * w.sinks * hkv * d * 4) : 0;
+  if (!parts) return 0;
+  const int64_t rows = ism::bwd_far_layout(batch, total, w.size, w.sinks).rows;
+  return align_up((size_t)2 * (near + parts) * rows * hkv * d * 4);
 }
 
 size_t bwd_part_bytes(int32_t batch, int32_t total, int32_t hq, int32_t hkv, int32_t d,
@@ -378,9 +382,12 @@ ism_status bwd_impl(const ism_segments *sg, const void *q, const void *k, const 
   if (!q || !k || !v || !o || !lse || !dout || !dq || !dk || !dv)
     return fail(ISM_ERR_NULL, "q, k, v, o, lse, dout, dq, dk, dv are required");
   if ((st = check_heads(hq, hkv, d, scale))) return st;
-  const size_t far_bytes = win ? bwd_far_bytes(sg->batch, sg->max_seqlen, hkv, d, *win) : 0;
-  const size_t need = bwd_min_workspace(sg->total_tokens, hq) + far_bytes;
-  if ((st = check_ws(ws, ws_bytes, need))) return st;
+  // (shared walks of the key tiles need no slot for the sinks' near rows)
+  auto far_bytes = [&](bool near) {
+    return win ? bwd_far_bytes(sg->batch, sg->total_tokens, sg->max_seqlen, hkv, d, *win, near) : 0;
+  };
+  const size_t base = bwd_min_workspace(sg->total_tokens, hq);
+  if ((st = check_ws(ws, ws_bytes, base + far_bytes(true)))) return st;
   const int32_t window = win ? win->size : 0;
   const size_t part_bytes = bwd_part_bytes(sg->batch, sg->total_tokens, hq, hkv, d, window);
   if ((st = check_device())) return st;
@@ -399,8 +406,8 @@ ism_status bwd_impl(const ism_segments *sg, const void *q, const void *k, const 
   ism::BwdArgs a{};
   a.q = q; a.k = k; a.v = v; a.o = o; a.dout = dout; a.lse = lse;
   a.dq = (float *)dq; a.dk = (float *)dk; a.dv = (float *)dv; a.lsex = lsex; a.deltax = deltax;
-  if (part_bytes && ws_bytes >= need + part_bytes) {
-    a.dkv_part = (float *)((char *)ws + need);
+  if (part_bytes && ws_bytes >= base + far_bytes(false) + part_bytes) {
+    a.dkv_part = (float *)((char *)ws + base + far_bytes(false));
     a.dkv_parts = ism::bwd_dkv_parts(sg->batch, sg->total_tokens, hq, hkv, window);
   }
   a.cu_seqlens = sg->cu_seqlens; a.cu_segs = sg->cu_segs;
@@ -413,7 +420,11 @@ ism_status bwd_impl(const ism_segments *sg, const void *q, const void *k, const 
     a.sinks = win->sinks;
     a.grad_bf16 = grad_dtype == ISM_DTYPE_BF16;
     a.far_parts = ism::bwd_far_parts(sg->batch, sg->max_seqlen, hkv, win->size, win->sinks);
-    a.far_part = (float *)((char *)ws + need - far_bytes);
+    a.far_part = (float *)((char *)ws + base);
+    const ism::FarLayout fl =
+        ism::bwd_far_layout(sg->batch, sg->total_tokens, win->size, win->sinks);
+    a.far_rows = (int32_t)fl.rows;
+    a.far_by = fl.by;
   }
   const hipError_t e = ism::launch_bwd(a, d, s);
   if (e == hipErrorNotSupported)
@@ -780,10 +791,11 @@ extern "C" size_t ism_attn_window_workspace_size(int32_t op, int32_t batch,
   switch (op) {
     case ISM_OP_FWD:
       return ism_attn_workspace_size(op, batch, total_tokens, max_seqlen, hq, hkv, d, 0);
-    case ISM_OP_BWD:
-      return bwd_min_workspace(total_tokens, hq) +
-             bwd_part_bytes(batch, total_tokens, hq, hkv, d, win.size) +
-             bwd_far_bytes(batch, max_seqlen, hkv, d, win);
+    case ISM_OP_BWD: {
+      const size_t parts = bwd_part_bytes(batch, total_tokens, hq, hkv, d, win.size);
+      return bwd_min_workspace(total_tokens, hq) + parts +
+             bwd_far_bytes(batch, total_tokens, max_seqlen, hkv, d, win, parts == 0);
+    }
     case ISM_OP_PREFILL_CACHED:
       return ism_attn_prefill_workspace_size(batch, total_tokens, max_new, hq, hkv, d,
                                              window_keys(win, max_new, max_seqlen));

@@ -23,7 +23,7 @@
 //     workgroups share a key tile's walk and a fourth kernel adds their
 //     partial dK and dV in order.
 // All products are bf16 MFMA 32x32x16 with fp32 accumulation; gradients are
-// written in fp32.
+// written in fp32 (windowed ones in bf16 if the caller asks for that).
 #include "ism_common.h"
 #include "ism_kernels.h"
 
@@ -122,6 +122,14 @@ __device__ __forceinline__ void product_stream(Rd &&rd, Mm &&mm, Mid &&mid) {
   }
 }
 
+// The first row of dialogue b, which starts at token s, in a slot of the sinks' partials
+// (FarLayout).
+__device__ __forceinline__ int64_t far_row(const BwdArgs &a, int b, int s) {
+  return a.far_by == kFarByToken   ? s
+         : a.far_by == kFarByStart ? (int64_t)(s / (a.window + 1)) * a.sinks
+                                   : (int64_t)b * a.sinks;
+}
+
 // Eight waves in four pairs; pair p owns the 32 keys c0 + 32 p (lane <->
 // key) and its two waves share one SIMD. Per 64-row tile t:
 //  * the P wave (p) computes S = Q K^T and P = exp(S - LSE) (masked),
@@ -187,7 +195,7 @@ dkv_kernel(BwdArgs a, int ktiles, int parts, int slots) {
     e = a.cu_seqlens[b + 1];
   }
   const int c0 = s + kt * kKW;
-  if (c0 >= e) return;
+  if (c0 >= e || (WIN && far && e - s <= a.window)) return;
   const int send = WIN ? min(s + a.sinks, e) : 0;  // end of the sinks
   const int kw0 = c0 + 32 * pair;
   const bool wactive = kw0 < e;
@@ -535,12 +543,13 @@ dkv_kernel(BwdArgs a, int ktiles, int parts, int slots) {
   float *base = pwave ? a.dv : a.dk;
   const float mul = pwave ? 1.f : a.scale;
   if constexpr (WIN) {
-    const bool sink = a.far_parts && key < send;
+    const bool sink = a.far_parts && key < send && e - s > a.window;
     if (far && !sink) return;
     if (far || (sink && parts == 1)) {  // a slot of the sinks' partials
-      const int64_t slot = (int64_t)(pwave ? 1 + a.far_parts : 0) + (far ? 1 + part : 0);
-      float *out = a.far_part + (((slot * a.batch + b) * a.sinks + (key - s)) * a.hkv + kvh) * D +
-                   hf * 4;
+      const int near = a.dkv_part ? 0 : 1;
+      const int64_t slot = (int64_t)(pwave ? near + a.far_parts : 0) + (far ? near + part : 0);
+      float *out = a.far_part +
+                   ((slot * a.far_rows + far_row(a, b, s) + (key - s)) * a.hkv + kvh) * D + hf * 4;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -591,22 +600,23 @@ dkv_sum_kernel(const float *__restrict__ part, float *__restrict__ dk, float *__
     ((f32x4 *)(second ? dv : dk))[o] = sum;
 }
 
-// Windowed attention: dK and dV of the sinks, the rows inside their window
-// (slot 0 of far_part, or the near workgroups' parts) and then the far parts,
-// in order and rounded once. A few hundred KB.
+// Windowed attention: dK and dV of the sinks that rows past their window see: the
+// rows inside it (the near slot of far_part, or the near workgroups' parts) and
+// then the far parts, in order and rounded once. An HBM stream of the partials, a
+// few hundred KB for a handful of sinks.
 __global__ void __launch_bounds__(256)
 win_sink_sum_kernel(BwdArgs a, int d, int parts) {
   const int64_t per = (int64_t)a.hkv * d / 4, tot4 = (int64_t)a.total * per;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int near = parts > 1 ? 0 : 1, slots = near + a.far_parts;
+  const int64_t step = a.far_rows * per;
   for (int b = blockIdx.y; b < a.batch; b += gridDim.y) {
-    const int s = a.cu_seqlens[b], n = min(a.sinks, a.cu_seqlens[b + 1] - s);
-    if (i >= 2 * n * per) continue;
+    const int s = a.cu_seqlens[b], e = a.cu_seqlens[b + 1], n = min(a.sinks, e - s);
+    if (e - s <= a.window || i >= 2 * n * per) continue;
     const bool second = i >= n * per;
     const int64_t o = second ? i - n * per : i, at = s * per + o;
-    const int slots = 1 + a.far_parts;
-    const f32x4 *far = (const f32x4 *)a.far_part +
-                       ((int64_t)(second ? slots : 0) * a.batch + b) * a.sinks * per + o;
-    const int64_t step = (int64_t)a.batch * a.sinks * per;
+    const f32x4 *far = (const f32x4 *)a.far_part + (second ? slots : 0) * step +
+                       far_row(a, b, s) * per + o;
     f32x4 sum = f32x4{};
     if (parts > 1) {
       const f32x4 *p = (const f32x4 *)a.dkv_part + (second ? parts * tot4 : 0) + at;
@@ -614,7 +624,7 @@ win_sink_sum_kernel(BwdArgs a, int d, int parts) {
     } else {
       sum = far[0];
     }
-    for (int j = 1; j < slots; ++j) sum += far[j * step];
+    for (int j = near; j < slots; ++j) sum += far[j * step];
     if (a.grad_bf16)
       ((u32x2 *)(second ? a.dv : a.dk))[at] =
           u32x2{pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3])};

@@ -236,19 +236,38 @@ struct BwdArgs {
   int32_t deterministic;
   // windowed attention (see FwdArgs). far_parts > 0: the rows past a sink's
   // window are walked by that many workgroups per key tile of sinks, which
-  // leave partial dK and dV in slots 1.. of far_part [2, 1 + far_parts, batch,
-  // sinks, hkv, d]; slot 0 takes the rows inside the window when dkv_part does
-  // not.
+  // leave partial dK and dV in far_part [2, near + far_parts, far_rows, hkv, d]
+  // (FarLayout). The slot in front of theirs (near = 1) takes the rows inside
+  // the window when dkv_part does not (near = 0).
   int32_t window, sinks, grad_bf16, far_parts;
   float *far_part;
+  int32_t far_rows, far_by;
   int32_t far_wgs;          // (set by the launch)
 };
 
+// The rows of a slot of the sinks' partials: only dialogues longer than the window
+// have any. At most total / (window + 1) are, and s / (window + 1) of their first
+// tokens s are all different and below that: kFarByStart gives the dialogue rows
+// from s / (window + 1) * sinks on. kFarByDialogue from b * sinks on, for few
+// dialogues; kFarByToken from s on, when that takes fewer rows than either.
+enum { kFarByDialogue = 0, kFarByStart = 1, kFarByToken = 2 };
+struct FarLayout {
+  int64_t rows;
+  int32_t by;
+};
+inline FarLayout bwd_far_layout(int batch, int total, int window, int sinks) {
+  FarLayout x{(int64_t)batch * sinks, kFarByDialogue};
+  const int64_t by_start = (int64_t)(total / (window + 1)) * sinks;
+  if (by_start < x.rows) x = FarLayout{by_start, kFarByStart};
+  if (total < x.rows) x = FarLayout{total, kFarByToken};
+  return x;
+}
+
 // Workgroups that share the walk of the rows past the sinks' window for each
 // key tile that holds sinks: as many as make it as long as any other tile's
-// walk, of up to window + 127 rows, but no more workgroups in all than 2048 while
-// there are fewer tiles than that (the partials are 8 sinks hkv d bytes each per
-// dialogue); none if no dialogue is longer than the window.
+// walk, of up to window + 127 rows, but at most 64, and no more workgroups in all
+// than 2048 while there are fewer tiles than that (the partials are 8 hkv d bytes
+// each per row of FarLayout); none if no dialogue is longer than the window.
 inline int bwd_far_parts(int batch, int max_seqlen, int hkv, int window, int sinks) {
   if (sinks < 1 || window >= max_seqlen) return 0;
   const int64_t far = max_seqlen - window, near = (int64_t)window + 128;
