@@ -470,7 +470,8 @@ __device__ __forceinline__ bool xcd_work_item(int bid, int groups, int tiles, in
 // set h are slots [first(b) + h n_b, + n_b), n_b >= their number (at most one more,
 // whose workgroup has nothing to do), first(b) = sets (floor(cu[b] / rows) + b);
 // XCD x takes a contiguous eighth of the slots. Returns false for ids past the
-// last slot; else the dialogue (with its tokens [s, e)), set and tile.
+// last slot, and past the last dialogue's if tokens behind it belong to none; else
+// the dialogue (with its tokens [s, e)), set and tile.
 __device__ __forceinline__ bool slot_work_item(int bid, int per_xcd, int slots, int sets, int rows,
                                                const int32_t *cu, int batch, int lane, int &b,
                                                int &s, int &e, int &set, int &tile) {
@@ -489,7 +490,7 @@ __device__ __forceinline__ bool slot_work_item(int bid, int per_xcd, int slots, 
   const int t0 = s / rows + b, n = e / rows + b + 1 - t0, r = slot - sets * t0;
   set = __builtin_amdgcn_readfirstlane(r / n);
   tile = __builtin_amdgcn_readfirstlane(r - set * n);
-  return true;
+  return set < sets;
 }
 
 // Grid size for xcd_work_item: 8 x the largest per-XCD item count.

@@ -54,13 +54,15 @@ fwd_window_kernel(FwdArgs a, int lf, int per_xcd, int slots) {
   };
   auto next_item = [&](WinItem &x) __attribute__((always_inline)) {
     for (; slot < slot_end; slot += stride) {
-      while (hsets * tiles_before(x.e, x.b + 1) <= slot) {
+      // (slots past the last dialogue's: tokens that belong to none)
+      while (x.b + 1 < a.batch && hsets * tiles_before(x.e, x.b + 1) <= slot) {
         ++x.b;
         x.s = x.e;
         x.e = a.cu_q[x.b + 1];
       }
       const int t0 = tiles_before(x.s, x.b), n = tiles_before(x.e, x.b + 1) - t0;
       const int r = slot - hsets * t0, h = __builtin_amdgcn_readfirstlane(r / n);
+      if (h >= hsets) break;
       x.c0 = __builtin_amdgcn_readfirstlane((r - h * n) * (NWV * kQW));
       x.head0 = h << lf;
       x.kv = (int64_t)x.s * rs + (int64_t)(x.head0 / kv_group) * a.kv_head_stride;
