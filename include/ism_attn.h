@@ -281,7 +281,8 @@ ism_status ism_attn_decode_paged(const void *q, const void *k_new,
  * long as the dialogue hides nothing. Keys that no row of a launch sees are
  * not visited, so time and cache traffic follow window and sinks, not the
  * dialogue's length. All other arguments, errors and conventions are those of
- * the operation without a window, with at most 2^30 positions to a dialogue.
+ * the operation without a window, with at most 2^30 positions to a dialogue, and
+ * tensors that are not 16-byte aligned (but lse) fail with ISM_ERR_UNSUPPORTED.
  * Workspaces: ism_attn_window_workspace_size, with `op` one of ISM_OP_*,
  * `total_tokens` the packed (or new) rows, `max_new` the longest new segment
  * (ISM_OP_PREFILL_CACHED only) and `max_seqlen` the longest dialogue
@@ -366,7 +367,8 @@ ism_status ism_attn_decode_paged_window(
  * to; a compaction moves pages to the front of the pool. src, dst and tokens
  * are device arrays of int32. A copy whose page index lies outside the pool
  * is left out. The copies of a call run in any order: no dst may be another
- * copy's src or dst. copies = 0 does nothing. page_size is any positive size. */
+ * copy's src or dst. copies = 0 does nothing. page_size is any positive size;
+ * the pools are 16-byte aligned. */
 ism_status ism_cache_copy_pages(void *k_pages, void *v_pages,
                                 int32_t num_pages, int32_t page_size,
                                 int32_t hkv, int32_t d, const int32_t *src,

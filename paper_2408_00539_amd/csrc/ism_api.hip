@@ -6,6 +6,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <initializer_list>
 #include <mutex>
 #include <vector>
 
@@ -225,6 +226,13 @@ ism_status check_window(Window &w, int32_t keys) {
   return ISM_OK;
 }
 
+// The kernels move 16 bytes at a time.
+ism_status check_aligned(std::initializer_list<const void *> tensors) {
+  for (const void *p : tensors)
+    if ((uintptr_t)p % 16) return fail(ISM_ERR_UNSUPPORTED, "a tensor is not 16-byte aligned");
+  return ISM_OK;
+}
+
 // Keys that the rows of a dialogue visit at most, in whole tiles of 64 (new
 // rows, keys in all), for the plans of split launches.
 int32_t window_keys(const Window &w, int32_t new_rows, int32_t keys) {
@@ -301,6 +309,7 @@ ism_status fwd_impl(const ism_segments *sg, const void *q, const void *k, const 
   if (win && (st = check_window(*win, sg->max_seqlen))) return st;
   if (!q || !k || !v || !o) return fail(ISM_ERR_NULL, "q, k, v and o are required");
   if ((st = check_heads(hq, hkv, d, scale))) return st;
+  if (win && (st = check_aligned({q, k, v, o}))) return st;
   const size_t need = ism_attn_workspace_size(ISM_OP_FWD, sg->batch, sg->total_tokens,
                                               sg->max_seqlen, hq, hkv, d, 0);
   if ((st = check_ws(ws, ws_bytes, need))) return st;
@@ -382,6 +391,7 @@ ism_status bwd_impl(const ism_segments *sg, const void *q, const void *k, const 
   if (!q || !k || !v || !o || !lse || !dout || !dq || !dk || !dv)
     return fail(ISM_ERR_NULL, "q, k, v, o, lse, dout, dq, dk, dv are required");
   if ((st = check_heads(hq, hkv, d, scale))) return st;
+  if (win && (st = check_aligned({q, k, v, o, dout, dq, dk, dv}))) return st;
   // (shared walks of the key tiles need no slot for the sinks' near rows)
   auto far_bytes = [&](bool near) {
     return win ? bwd_far_bytes(sg->batch, sg->total_tokens, sg->max_seqlen, hkv, d, *win, near) : 0;
@@ -528,6 +538,7 @@ ism_status prefill_impl(const int32_t *cu_seqlens_new, int32_t batch, int32_t to
   Window win{0, 0};
   if (window) {
     win = *window;
+    if ((st = check_aligned({q_new, k_new, v_new, k_cache, v_cache, o}))) return st;
     if ((st = check_window(win, cache_cap))) return st;
   }
   if (rp) {
@@ -724,6 +735,7 @@ ism_status decode_impl(const void *q, const void *k_new, const void *v_new, void
   Window win{0, 0};
   if (window) {
     win = *window;
+    if ((st = check_aligned({q, k_new, v_new, k_cache, v_cache, o}))) return st;
     if ((st = check_window(win, cache_cap))) return st;
     max_seqlen = window_keys(win, 1, max_seqlen);
   }
@@ -870,10 +882,11 @@ extern "C" ism_status ism_cache_copy_pages(void *k_pages, void *v_pages, int32_t
                 "%d)", copies, num_pages, page_size, hkv);
   if (d != 64 && d != 128)
     return fail(ISM_ERR_UNSUPPORTED, "head dim %d not supported (64 or 128)", d);
+  ism_status st = check_aligned({k_pages, v_pages});
+  if (st) return st;
   if ((int64_t)page_size * d > INT32_MAX / 2)
     return fail(ISM_ERR_SHAPE, "page_size %d too large", page_size);
-  ism_status st = check_device();
-  if (st) return st;
+  if ((st = check_device())) return st;
   return hip_status(ism::launch_copy_pages(k_pages, v_pages, num_pages, page_size, hkv, d, src,
                                            dst, tokens, copies, (hipStream_t)stream),
                     "page copy launch");
