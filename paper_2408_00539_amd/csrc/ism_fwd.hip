@@ -57,7 +57,11 @@ namespace {
 // spread 2320, eight waves 2312; pages of 256 2260, 2142, 2209; 40 over 20 x
 // 8000, pages of 64 272, 235, 229); on short ones, where a tile's latency is
 // hidden by little else, an early start wins (64 over 40 x 2000, pages of 64
-// 133, spread 156).
+// 133, spread 156). Under a window it is the window's length that counts, and less
+// hangs on it, pages of 64: window 8192, at the step start and spread, 300 over 8 x
+// 20000, 32/8 heads 438, 436; 40 over 40 x 12000 509, 470; but 64 over 20 x 20000,
+// 32 heads 506, 562; 16/4 heads, d 64 148, 148; window 16384, 1000 over 4 x 40000
+// 1141, 1147; window 4096, 300 over 8 x 20000 245, 245; 40 over 40 x 12000 261, 236.
 constexpr int kSpreadKeys = 8192;
 
 // NT: non-temporal tile transfers, for a cache-mode launch in which every
