@@ -306,7 +306,10 @@ ism_status ism_attn_fwd_window(const ism_segments *sg, const void *q,
 /* Its backward (ism_attn_bwd; bitwise repeatable, no atomics). dq, dk and dv
  * are all fp32 or all bf16 (grad_dtype, ISM_DTYPE_F32 or ISM_DTYPE_BF16); the
  * sums are fp32 either way and a bf16 gradient is rounded once, when it is
- * complete. */
+ * complete. The workspace holds partial dK and dV of the sinks of dialogues
+ * longer than the window: at most twice the fp32 dK and dV or 403 MB, whichever
+ * is more. ISM_OP_BWD's size also has room for shared walks on calls of few
+ * tokens, and a workspace without it runs them unshared, as in ism_attn_bwd. */
 ism_status ism_attn_bwd_window(const ism_segments *sg, const void *q,
                                const void *k, const void *v, const void *o,
                                const float *lse, const void *dout, void *dq,
@@ -318,12 +321,13 @@ ism_status ism_attn_bwd_window(const ism_segments *sg, const void *q,
 /* New segment against a cache (ism_attn_prefill_cached_segment,
  * ism_attn_prefill_paged): row r of dialogue b sits at position C_b + r. Cached
  * positions that no new row sees ([sinks, C_b - window + 1)) are not read,
- * whatever they hold, nor are the block table's entries of pages that lie
- * wholly inside that range: those pages may have been freed. (Dense and paged
+ * whatever they hold, and the block table's entries of pages that lie wholly
+ * inside that range are not followed: those pages may have been freed. (Dense and paged
  * caches give the same results to rounding: their tiles start at other keys.)
  * A key whose K or
  * V is not finite makes the rows that see it non-finite, and possibly other
- * new rows of its dialogue. */
+ * new rows of its dialogue. The prefill with fused 2-D rotation has no windowed
+ * form: rotate q_new and k_new with ism_rope2d first. */
 ism_status ism_attn_prefill_window(
     const int32_t *cu_seqlens_new, int32_t batch, int32_t total_new,
     int32_t max_new, int32_t seg_is_query, const void *q_new,
@@ -343,7 +347,9 @@ ism_status ism_attn_prefill_paged_window(
 
 /* One decode step (ism_attn_decode, ism_attn_decode_paged): the new token at
  * p_b sees [0, sinks) and (p_b - window, p_b]. Nothing else of the cache is
- * read (pages as for the prefill). */
+ * read (pages as for the prefill). There is no form without a workspace:
+ * ism_attn_window_workspace_size does not depend on the lengths, so that a
+ * caller under graph capture can hold one of it. */
 ism_status ism_attn_decode_window(
     const void *q, const void *k_new, const void *v_new, void *k_cache,
     void *v_cache, int32_t cache_cap, const int32_t *cache_seqlens,

@@ -739,7 +739,12 @@ ism_status decode_impl(const void *q, const void *k_new, const void *v_new, void
     if ((st = check_window(win, cache_cap))) return st;
     max_seqlen = window_keys(win, 1, max_seqlen);
   }
-  // (a windowed step always takes the split-key kernel)
+  // A windowed step always takes the split-key kernel. On the sizes for which a step
+  // without a window takes the vector kernel, that one and this under a window over
+  // as many keys (us): 32 dialogues x 4000 keys, 32 heads 386, 362; 64 x 4000, 16
+  // heads, d 64 161, 166; 16/8 heads 168, 166; 16 x 12000, 32 heads 467, 461; but
+  // 64 x 8000, 32/16 heads 616, 661; 32 x 1000, 32 heads 82, 91; 128 x 500, 8 heads
+  // 44, 50.
   const bool vec = !window && ism::decode_vector(batch, hq, hkv);
   const size_t need = window ? window_decode_bytes(batch, max_seqlen, hq, hkv, d, num_splits)
                              : decode_min_workspace(batch, max_seqlen, hq, hkv, d, num_splits);

@@ -84,7 +84,11 @@ constexpr int kDkvStages = 3;
 // consecutive lanes touch consecutive bytes). fp16 rather than bf16: P lies
 // in [0, 1], where fp16 keeps 3 more mantissa bits, so the dS wave's
 // dS = P o (dP - delta) carries one rounding of P 8x smaller than bf16's,
-// and its fp16 x fp32 products are single v_fma_mix_f32 instructions.
+// and its fp16 x fp32 products are single v_fma_mix_f32 instructions. What enters
+// the products over rows, P for dV and dS for dK (and for dQ in its kernel), is
+// rounded to one bf16 each: dQ, dK and dV are off by about 0.0024 of their norms with
+// bf16 gradients (0.0017 of that their own rounding), and two summands would add
+// half of those products again, with the matrix core the bound.
 template <int D>
 struct DkvSmem {
   bf16_t q[kDkvStages][kBR * D];

@@ -126,7 +126,10 @@ __device__ __forceinline__ void raise_max(float mt, float sl2, float tau, float 
 // the S products the exponentials, row sums and bf16 packing of tile t,
 // during the P V products the row max of S(t+1). The order is pinned with
 // scheduling barriers so that the matrix core and the vector ALU of a wave
-// are busy at the same time. Returns the fp32 row sum of P(t); mt receives
+// are busy at the same time. P enters the second product rounded to bf16 (o is
+// off by 0.0020 to 0.0023 of its norm, by its own rounding alone 0.0017): as two
+// bf16 summands it would take half as many products again, where the matrix core
+// is the bound. Returns the fp32 row sum of P(t); mt receives
 // the (unmasked) row max of S(t+1). With LAST (a wave's last tile) there is
 // no S(t+1): the exponentials run alone, then the P V products.
 // With PRIO the wave raises its issue priority for the first half (the S

@@ -68,7 +68,10 @@ hipError_t launch_fwd_window(const FwdArgs &a, int d, hipStream_t stream);
 // kernel against it (us): 12 dialogues up to 3000 tokens, 32/8 heads, window
 // 512 346, 253; 1024 453, 341; 32 heads 333, 312 and 409, 398; 4 x 8192, 32/8
 // heads 424, 384 and 597, 569; 32 heads 506, 479 and 682, 679, but window 2048
-// 1043, 1064; 6 ragged up to 900, 16/4 heads, d 64, window 201 14.4, 17.1.
+// 1043, 1064; 6 ragged up to 900, 16/4 heads, d 64, window 201 14.4, 17.1. Whole
+// passes above 1024: 4 x 8192, 32/8 heads, window 1500 781, 779; 2048 959, 947; 4096
+// 1504, 1543; 2 x 16384, 2048 1013, 1000; 8 x 4096, 2048 824, 864; 4 x 8192, 32 heads,
+// 1500 877, 890; 2048 1072, 1106; 16/8 heads, d 64, 2048 291, 306.
 inline bool fwd_window_items(const FwdArgs &a) {
   const bool equal = (int64_t)a.total_q * 10 >= (int64_t)a.batch * a.max_rows * 9;
   return a.lim && (!equal || a.window <= 1024);

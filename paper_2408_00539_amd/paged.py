@@ -25,7 +25,10 @@ entry points (``ops.prefill_paged``, ``ops.decode_paged``):
 With ``window`` (and ``sinks``) the attention is windowed
 (``ops.prefill_paged_window``, ``ops.decode_paged_window``), and pages that lie
 behind the window of every later token, and hold no sink, return to the pool
-as the dialogue grows.
+as the dialogue grows. A rollback to before such pages were freed is refused: to
+answer a turn again, ``fork`` the dialogue before its answer is appended (the fork
+keeps what it sees). Positions go on counting from the dialogue's first token, so
+that it still ends at ``max_pages * page_size`` of them.
 
 ``PageAllocator`` is the host-side bookkeeping (no GPU): a free list of page
 indices, the number of slots that hold each page, and each dialogue slot's
