@@ -296,7 +296,9 @@ size_t ism_attn_window_workspace_size(int32_t op, int32_t batch,
                                       int32_t hkv, int32_t d, int32_t window,
                                       int32_t sinks, int32_t num_splits);
 
-/* Forward over packed dialogues (ism_attn_fwd). */
+/* Forward over packed dialogues (ism_attn_fwd). A token whose K or V is not
+ * finite makes the rows that see it non-finite, and possibly other rows of its
+ * dialogue; no other dialogue's. */
 ism_status ism_attn_fwd_window(const ism_segments *sg, const void *q,
                                const void *k, const void *v, void *o,
                                float *lse, int32_t hq, int32_t hkv, int32_t d,
